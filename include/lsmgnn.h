@@ -530,7 +530,8 @@ lsmgnn_status lsmgnn_route_combine_grad(const void *dy, uint64_t n, uint64_t dim
      lsmgnn_act8_grad  dx = dy * f'(x^) from the kept values x^; gated:
                      da = dy * b^ * f'(a^) and db = dy * f(a^), side by side.
    act: LSMGNN_SILU, f(x) = x / (1 + exp(-x)); LSMGNN_GELU, f(x) = x Phi(x) with
-   the normal distribution function. */
+   the normal distribution function; f(-inf) is NaN.  Products with f and f' are
+   infinite only where their value is past the type's range. */
 #define LSMGNN_PACK_BLOCK 32u
 #define LSMGNN_SILU 0u
 #define LSMGNN_GELU 1u

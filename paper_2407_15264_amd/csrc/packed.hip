@@ -135,35 +135,45 @@ __device__ __forceinline__ void kept8(const int8_t *q, const uint8_t *scale, int
   for (int e = 0; e < kLane; ++e) v[e] = (float)t[e] * unit;
 }
 
-// exp(-a) = e 2^n for a >= 0, e to about the last bit in [0.7, 1.5]: a log2(e) in two
-// parts.  Beyond the clamp the result is 0 all the same.
+// exp(-a) = e 2^n for 0 <= a <= 800, e to about the last bit in [0.7, 1.5]: a log2(e) in
+// two parts.
 __device__ __forceinline__ float exp_neg(float a, int *n) {
 #pragma clang fp contract(off)
-  a = fminf(a, 400.0f);
   const float whole = rintf(a * -1.44269504088896340736f);
   const float part = __builtin_fmaf(a, -1.9259629911266175e-8f, __builtin_fmaf(a, -1.44269504088896340736f, -whole));
   *n = (int)whole;
   return __builtin_amdgcn_exp2f(part);
 }
 
+// A factor as m 2^up, 0.5 <= |m| < 1 (0, infinities and NaNs as they are, up = 0): a
+// product of such mantissas neither overflows nor underflows before its exponents
+// are added to it.
+__device__ __forceinline__ float mantissa(float v, int *up) {
+  *up += __builtin_amdgcn_frexp_expf(v);
+  return __builtin_amdgcn_frexp_mantf(v);
+}
+
 // f(x) and f'(x), both to be multiplied by 2^up at last, so that a product with
 // another factor is rounded once where it is subnormal.  kFull: to a few units of
-// the last place of a float; else the reciprocal's own error stays.
+// the last place of a float; else the reciprocal's own error stays.  f(-inf) is NaN, as
+// in x / (1 + exp(-x)).
 template <uint32_t kAct, bool kFull>
 __device__ __forceinline__ void act(float x, float *f, float *df, int *up) {
   int n;
   if (kAct == LSMGNN_SILU) {
-    // p = 1 / (1 + exp(-x)) and 1 - p from t = exp(-|x|), which cannot overflow
-    const float e = exp_neg(fabsf(x), &n), t = __builtin_amdgcn_ldexpf(e, n), d = 1.0f + t;
+    // p = 1 / (1 + exp(-x)) and 1 - p from t = exp(-|x|), which cannot overflow; beyond
+    // 400 it is 0 to any factor a float can have, and v keeps x p 2^-up finite there
+    const float y = fminf(fabsf(x), 400.0f), v = x < 0.0f ? __builtin_fmaf(x, 0.0f, -y) : x;
+    const float e = exp_neg(y, &n), t = __builtin_amdgcn_ldexpf(e, n), d = 1.0f + t;
     float r = __builtin_amdgcn_rcpf(d);
     if (kFull) r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
     const float p = x < 0.0f ? e * r : r, rest = x < 0.0f ? r : t * r;
     *up = x < 0.0f ? n : 0;
-    *f = x * p;
-    *df = p * __builtin_fmaf(x, rest, 1.0f);
+    *f = v * p;
+    *df = p * __builtin_fmaf(v, rest, 1.0f);
   } else {
     const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
-    const float e = exp_neg(0.5f * x * x, &n);
+    const float e = exp_neg(fminf(0.5f * x * x, 400.0f), &n);
     *f = x * cdf;
     *df = __builtin_fmaf(x, __builtin_amdgcn_ldexpf(e, n) * 0.39894228040143268f, cdf);
     *up = 0;
@@ -208,7 +218,8 @@ __global__ __launch_bounds__(kBlock) void k_act(Cut c, const T *x, uint64_t xld,
       float f, df;
       int up;
       act<kAct, sizeof(T) == 4>(a[u][e], &f, &df, &up);
-      o[e] = __builtin_amdgcn_ldexpf(kGated ? f * b[u][e] : f, up);
+      if (kGated) f *= mantissa(b[u][e], &up);
+      o[e] = __builtin_amdgcn_ldexpf(f, up);
     }
     if (p[u].count) store8(y + p[u].row * yld + p[u].col, p[u].count, o);
     int8_t *qp = q + p[u].row * kRows * c.dim + p[u].col;
@@ -241,8 +252,10 @@ __global__ __launch_bounds__(kBlock) void k_act_grad(Cut c, const T *dy, uint64_
       float f, df;
       int up;
       act<kAct, sizeof(T) == 4>(a[u][e], &f, &df, &up);
-      o[e] = __builtin_amdgcn_ldexpf(kGated ? g[u][e] * b[u][e] * df : g[u][e] * df, up);
-      if (kGated) b[u][e] = __builtin_amdgcn_ldexpf(g[u][e] * f, up);
+      const float m = mantissa(g[u][e], &up);
+      int up_b = up;
+      o[e] = __builtin_amdgcn_ldexpf(kGated ? m * mantissa(b[u][e], &up_b) * df : m * df, up_b);
+      if (kGated) b[u][e] = __builtin_amdgcn_ldexpf(m * f, up);
     }
     if (p[u].count == 0) continue;
     T *to = dx + p[u].row * dxld + p[u].col;

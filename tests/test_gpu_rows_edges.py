@@ -1,0 +1,89 @@
+"""The operators on trained rows at the ends of their ranges, against 64-bit
+references on the GPU."""
+import numpy as np
+import pytest
+
+from tests import rows_reference as ref
+from tests.test_gpu_embed import TYPES, rows
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2407_15264_amd import lsmgnn  # noqa: E402
+
+LEAST = 2.0 ** -149  # a float32's spacing next to 0: a product rounded once more where it is subnormal
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    lsmgnn.lib()
+
+
+def dev(a, dtype=torch.float32):
+    return torch.as_tensor(np.ascontiguousarray(a), dtype=torch.float64).to(dtype).cuda()
+
+
+# --------------------------------------- gated activations of numbers far apart
+A_FAR = [-1e30, -1000.0, -400.0, -300.0, -200.0, -104.0, -90.0, -87.0, -50.0, -10.0, -3.0, -1.0, -0.25, 0.0, 0.5, 1.0]
+SIZES = [1e38, 1e36, 1e25, 1e20, 1e10, 1.0, 1e-10, 1e-30]
+
+
+def far_rows(dtype, rng=None, n=0):
+    """(a, b, dy) of every combination of A_FAR and SIZES, and n drawn ones, as
+    the type holds them, where the 64-bit results fit in it."""
+    a, b, g = (v.reshape(-1) for v in np.meshgrid(A_FAR, SIZES + [-v for v in SIZES], SIZES, indexing="ij"))
+    if n:
+        sign = lambda: rng.choice([-1.0, 1.0], n)  # noqa: E731
+        a = np.concatenate([a, -10.0 ** rng.uniform(-2, 2.8, n)])
+        b = np.concatenate([b, sign() * 10.0 ** rng.uniform(-37, 38, n)])
+        g = np.concatenate([g, sign() * 10.0 ** rng.uniform(-37, 38, n)])
+    return [ref.f64(dev(v, dtype)).reshape(-1, 1) for v in (a, b, g)]
+
+
+def check_far(dtype, act, forward, slope):
+    a, b, g = far_rows(dtype, np.random.default_rng(1), 20000)
+    ka, kb = ref.pack(a)[2], ref.pack(b)[2]
+    f, bf = forward(a)
+    kf, bkf = forward(ka)
+    kdf, bdf = slope(ka)
+    fits = np.abs(np.stack([f * b, g * kb * kdf, g * kf])).max(0)[:, 0] < 3e38
+    a, b, g, kb, f, bf, kf, bkf, kdf, bdf = (v[fits] for v in (a, b, g, kb, f, bf, kf, bkf, kdf, bdf))
+    assert a.shape[0] > 15000
+    y, p = lsmgnn.act8(dev(np.concatenate([a, b], 1), dtype), act, True)
+    ref.assert_within(y, f * b, (bf + 2 * ref.U32 * np.abs(f)) * np.abs(b) + LEAST, dtype, "y")
+    dx = lsmgnn.act8_grad(dev(g, dtype), p, act, True)
+    ref.assert_within(dx[:, :1], g * kb * kdf, np.abs(g * kb) * (bdf + 3 * ref.U32 * np.abs(kdf)) + LEAST, dtype, "da")
+    ref.assert_within(dx[:, 1:], g * kf, np.abs(g) * (bkf + 2 * ref.U32 * np.abs(kf)) + LEAST, dtype, "db")
+    # without a gate
+    _, p = lsmgnn.act8(dev(a, dtype), act)
+    fits = np.abs(g * kdf)[:, 0] < 3e38
+    dx = lsmgnn.act8_grad(dev(g, dtype), p, act)
+    ref.assert_within(dx[torch.as_tensor(fits).cuda()], (g * kdf)[fits],
+                      (np.abs(g) * (bdf + 2 * ref.U32 * np.abs(kdf)) + LEAST)[fits], dtype, "dx")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_silu_with_large_and_small_factors(dtype):
+    """Finite inputs with finite results: none of the products on the way leaves
+    the range of a float."""
+    check_far(dtype, "silu", lambda x: ref.act("silu", x)[:2], lambda x: ref.act("silu", x)[2:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ["silu"])
+def test_activation_of_infinities(dtype, act):
+    """f(inf) = inf; f(-inf) is what the formula is there, NaN."""
+    x = torch.tensor([[float("inf")], [-float("inf")], [float("nan")], [1.0]], device="cuda").to(dtype)
+    y = lsmgnn.act8(x, act)[0].cpu()
+    assert y[0, 0] == float("inf") and torch.isnan(y[1:3]).all() and torch.isfinite(y[3, 0])
+    for b in (2.0, -2.0):
+        gate = torch.full_like(x, b)
+        y = lsmgnn.act8(torch.cat([x, gate], 1), act, True)[0].cpu()
+        assert y[0, 0] == b * float("inf") and torch.isnan(y[1:3]).all() and torch.isfinite(y[3, 0])
+    # an infinite gate of an ordinary value
+    y = lsmgnn.act8(torch.tensor([[-3.0, float("inf")], [-1000.0, float("inf")], [2.0, -float("inf")]],
+                                 device="cuda").to(dtype), act, True)[0].cpu()
+    assert (y == -float("inf")).all()
