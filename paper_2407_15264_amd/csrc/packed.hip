@@ -88,20 +88,28 @@ __device__ __forceinline__ void store8(T *p, int count, const float (&v)[kLane])
   }
 }
 
-// Keep a block's values: its lanes' quotients at q, the scale byte by its first
-// lane.  Every lane of the wave calls it.
-__device__ __forceinline__ void keep8(const float (&v)[kLane], const Place &p, int8_t *q, uint8_t *scale) {
+constexpr uint32_t kInf = 0x7f800000u;  // a float's bits
+
+// The largest magnitude's bits.
+__device__ __forceinline__ uint32_t largest(const float (&v)[kLane]) {
   uint32_t big = 0;
 #pragma unroll
   for (int e = 0; e < kLane; ++e) {
     const uint32_t m = __float_as_uint(v[e]) & 0x7fffffffu;
     big = m > big ? m : big;
   }
+  return big;
+}
+
+// Keep a block's values: its lanes' quotients at q, the scale byte by its first
+// lane.  Every lane of the wave calls it.
+__device__ __forceinline__ void keep8(const float (&v)[kLane], const Place &p, int8_t *q, uint8_t *scale) {
+  uint32_t big = largest(v);
   const uint32_t a = __shfl_xor(big, 1);
   big = a > big ? a : big;
   const uint32_t b = __shfl_xor(big, 2);
   big = b > big ? b : big;
-  const bool fine = big < 0x7f800000u;
+  const bool fine = big < kInf;
   const int32_t field = (int32_t)((big + 0x10000u) >> 23) - 6;  // s + 127
   const uint32_t byte = !fine ? 255u : field < 1 ? 1u : (uint32_t)field;
   const float per_unit = __uint_as_float((254u - byte) << 23);  // 2^-s
@@ -136,48 +144,91 @@ __device__ __forceinline__ void kept8(const int8_t *q, const uint8_t *scale, int
 }
 
 // exp(-a) = e 2^n for 0 <= a <= 800, e to about the last bit in [0.7, 1.5]: a log2(e) in
-// two parts.
-__device__ __forceinline__ float exp_neg(float a, int *n) {
+// two parts.  kRest: of a + rest, |rest| <= 2^-24 a.
+template <bool kRest = false>
+__device__ __forceinline__ float exp_neg(float a, int *n, float rest = 0.0f) {
 #pragma clang fp contract(off)
   const float whole = rintf(a * -1.44269504088896340736f);
-  const float part = __builtin_fmaf(a, -1.9259629911266175e-8f, __builtin_fmaf(a, -1.44269504088896340736f, -whole));
+  float part = __builtin_fmaf(a, -1.9259629911266175e-8f, __builtin_fmaf(a, -1.44269504088896340736f, -whole));
+  if (kRest) part = __builtin_fmaf(rest, -1.44269504088896340736f, part);
   *n = (int)whole;
   return __builtin_amdgcn_exp2f(part);
 }
 
+// Products of activations with other factors.  A float16 row's values, and their
+// products, are far from a float's limits; those of the other types are not.
+template <typename T>
+constexpr bool kWide = !std::is_same<T, _Float16>::value;
+
 // A factor as m 2^up, 0.5 <= |m| < 1 (0, infinities and NaNs as they are, up = 0): a
 // product of such mantissas neither overflows nor underflows before its exponents
 // are added to it.
+template <typename T>
 __device__ __forceinline__ float mantissa(float v, int *up) {
+  if (!kWide<T>) return v;
   *up += __builtin_amdgcn_frexp_expf(v);
   return __builtin_amdgcn_frexp_mantf(v);
 }
 
-// f(x) and f'(x), both to be multiplied by 2^up at last, so that a product with
-// another factor is rounded once where it is subnormal.  kFull: to a few units of
-// the last place of a float; else the reciprocal's own error stays.  f(-inf) is NaN, as
-// in x / (1 + exp(-x)).
-template <uint32_t kAct, bool kFull>
+template <typename T>
+__device__ __forceinline__ float scaled(float v, int up) {
+  return kWide<T> ? __builtin_amdgcn_ldexpf(v, up) : v;
+}
+
+// exp(y^2 / 2) Phi(-y) = exp(y^2 / 2) erfc(y / sqrt 2) / 2 for 0 <= y <= 32, r times a
+// polynomial in 1 - 8 r, r = 1 / (y + 4): fitted to the function for the least relative
+// error, 1.6e-8.  In 32 bits, everywhere: 10 units of 2^-24 with the reciprocal's own
+// error, 7 where kFull takes that away.
+template <bool kFull>
+__device__ __forceinline__ float scaled_tail(float y) {
+  const float d = y + 4.0f;
+  float r = __builtin_amdgcn_rcpf(d);
+  if (kFull) r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+  const float t = __builtin_fmaf(-8.0f, r, 1.0f);
+  float q = -1.569715823e-04f;
+  q = __builtin_fmaf(q, t, 1.337611611e-04f);
+  q = __builtin_fmaf(q, t, 1.567938598e-03f);
+  q = __builtin_fmaf(q, t, -3.480502637e-03f);
+  q = __builtin_fmaf(q, t, -7.516742218e-03f);
+  q = __builtin_fmaf(q, t, 6.039651111e-02f);
+  q = __builtin_fmaf(q, t, -1.865253896e-01f);
+  q = __builtin_fmaf(q, t, 3.871374726e-01f);
+  q = __builtin_fmaf(q, t, -6.078965068e-01f);
+  q = __builtin_fmaf(q, t, 7.552851439e-01f);
+  return r * q;
+}
+
+// f(x) and f'(x) of a finite x or a NaN, both to be multiplied by 2^up at last (0 if not
+// kWide), so that a product with another factor is rounded once where it is subnormal.
+// To 16 units of 2^-24 where x is negative and they are small, too (Phi from 1 + erf
+// would lose all of them at -5.5); with 32-bit rows the reciprocals' own error is taken
+// away and that of gelu's square, x^2 / 2 units in its tail, which 16 bits do not show.
+template <uint32_t kAct, typename T>
 __device__ __forceinline__ void act(float x, float *f, float *df, int *up) {
+  constexpr bool kFull = sizeof(T) == 4;
+  // past these |x|, where a is 400 or 512, exp(-a) is 0 to any factor a float can have
+  const float y = fminf(fabsf(x), kAct == LSMGNN_SILU ? 400.0f : 32.0f);
   int n;
   if (kAct == LSMGNN_SILU) {
-    // p = 1 / (1 + exp(-x)) and 1 - p from t = exp(-|x|), which cannot overflow; beyond
-    // 400 it is 0 to any factor a float can have, and v keeps x p 2^-up finite there
-    const float y = fminf(fabsf(x), 400.0f), v = x < 0.0f ? __builtin_fmaf(x, 0.0f, -y) : x;
+    // p = 1 / (1 + exp(-x)) and 1 - p from t = exp(-|x|), which cannot overflow
     const float e = exp_neg(y, &n), t = __builtin_amdgcn_ldexpf(e, n), d = 1.0f + t;
     float r = __builtin_amdgcn_rcpf(d);
     if (kFull) r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
-    const float p = x < 0.0f ? e * r : r, rest = x < 0.0f ? r : t * r;
-    *up = x < 0.0f ? n : 0;
-    *f = v * p;
-    *df = p * __builtin_fmaf(v, rest, 1.0f);
+    const float p = x < 0.0f ? (kWide<T> ? e : t) * r : r, rest = x < 0.0f ? r : t * r;
+    *f = x * p;
+    *df = p * __builtin_fmaf(x, rest, 1.0f);
   } else {
-    const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
-    const float e = exp_neg(fminf(0.5f * x * x, 400.0f), &n);
-    *f = x * cdf;
-    *df = __builtin_fmaf(x, __builtin_amdgcn_ldexpf(e, n) * 0.39894228040143268f, cdf);
-    *up = 0;
+    // Phi(-y) = exp(-a) tail and the density exp(-a) 0.3989.. with a = y^2 / 2: x Phi(-y) and
+    // Phi(-y) - y density are f and f' where x < 0, else what x and 1 have more than f and f'
+    const float half = 0.5f * y, a = half * y;
+    const float e = exp_neg<kFull>(a, &n, kFull ? __builtin_fmaf(half, y, -a) : 0.0f);
+    const float tail = scaled_tail<kFull>(y);
+    const float s = kWide<T> ? e : __builtin_amdgcn_ldexpf(e, n);
+    const float less = y * (s * tail), dless = s * __builtin_fmaf(fabsf(x), -0.39894228040143268f, tail);
+    *f = x < 0.0f ? -less : x - scaled<T>(less, n);
+    *df = x < 0.0f ? dless : 1.0f - scaled<T>(dless, n);
   }
+  *up = kWide<T> && x < 0.0f ? n : 0;
 }
 
 template <typename T>
@@ -217,10 +268,22 @@ __global__ __launch_bounds__(kBlock) void k_act(Cut c, const T *x, uint64_t xld,
     for (int e = 0; e < kLane; ++e) {
       float f, df;
       int up;
-      act<kAct, sizeof(T) == 4>(a[u][e], &f, &df, &up);
-      if (kGated) f *= mantissa(b[u][e], &up);
-      o[e] = __builtin_amdgcn_ldexpf(f, up);
+      act<kAct, T>(a[u][e], &f, &df, &up);
+      // gelu's f is below 1, or x >= 0: its product with the gate needs no mantissa
+      const float gate = !kGated ? 1.0f : kAct == LSMGNN_GELU ? b[u][e] : mantissa<T>(b[u][e], &up);
+      o[e] = scaled<T>(kGated ? f * gate : f, up);
     }
+    // f(inf) = inf, f(-inf) is the formulas' NaN; an infinite gate of an f that is 0 in
+    // 32 bits alone
+    if (largest(a[u]) >= kInf || (kGated && largest(b[u]) >= kInf))
+#pragma unroll
+      for (int e = 0; e < kLane; ++e) {
+        const float x = a[u][e], gate = kGated ? b[u][e] : 1.0f;
+        if (fabsf(x) == __builtin_inff())
+          o[e] = (x > 0.0f ? x : __builtin_nanf("")) * gate;
+        else if (kGated && fabsf(gate) == __builtin_inff())
+          o[e] = x * gate;
+      }
     if (p[u].count) store8(y + p[u].row * yld + p[u].col, p[u].count, o);
     int8_t *qp = q + p[u].row * kRows * c.dim + p[u].col;
     uint8_t *sp = scale + p[u].row * kRows * c.nb + p[u].block;
@@ -251,11 +314,11 @@ __global__ __launch_bounds__(kBlock) void k_act_grad(Cut c, const T *dy, uint64_
     for (int e = 0; e < kLane; ++e) {
       float f, df;
       int up;
-      act<kAct, sizeof(T) == 4>(a[u][e], &f, &df, &up);
-      const float m = mantissa(g[u][e], &up);
+      act<kAct, T>(a[u][e], &f, &df, &up);
+      const float m = mantissa<T>(g[u][e], &up);
       int up_b = up;
-      o[e] = __builtin_amdgcn_ldexpf(kGated ? m * mantissa(b[u][e], &up_b) * df : m * df, up_b);
-      if (kGated) b[u][e] = __builtin_amdgcn_ldexpf(m * f, up);
+      o[e] = scaled<T>(kGated ? m * mantissa<T>(b[u][e], &up_b) * df : m * df, up_b);
+      if (kGated) b[u][e] = scaled<T>(m * f, up);
     }
     if (p[u].count == 0) continue;
     T *to = dx + p[u].row * dxld + p[u].col;

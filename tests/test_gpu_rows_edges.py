@@ -55,7 +55,8 @@ def check_far(dtype, act, forward, slope):
     y, p = lsmgnn.act8(dev(np.concatenate([a, b], 1), dtype), act, True)
     ref.assert_within(y, f * b, (bf + 2 * ref.U32 * np.abs(f)) * np.abs(b) + LEAST, dtype, "y")
     dx = lsmgnn.act8_grad(dev(g, dtype), p, act, True)
-    ref.assert_within(dx[:, :1], g * kb * kdf, np.abs(g * kb) * (bdf + 3 * ref.U32 * np.abs(kdf)) + LEAST, dtype, "da")
+    ref.assert_within(dx[:, :1], g * kb * kdf, np.abs(g * kb) * (bdf + 3 * ref.U32 * np.abs(kdf)) + LEAST, dtype,
+                      "da")
     ref.assert_within(dx[:, 1:], g * kf, np.abs(g) * (bkf + 2 * ref.U32 * np.abs(kf)) + LEAST, dtype, "db")
     # without a gate
     _, p = lsmgnn.act8(dev(a, dtype), act)
@@ -73,7 +74,7 @@ def test_silu_with_large_and_small_factors(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("act", ["silu"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_activation_of_infinities(dtype, act):
     """f(inf) = inf; f(-inf) is what the formula is there, NaN."""
     x = torch.tensor([[float("inf")], [-float("inf")], [float("nan")], [1.0]], device="cuda").to(dtype)
@@ -87,3 +88,40 @@ def test_activation_of_infinities(dtype, act):
     y = lsmgnn.act8(torch.tensor([[-3.0, float("inf")], [-1000.0, float("inf")], [2.0, -float("inf")]],
                                  device="cuda").to(dtype), act, True)[0].cpu()
     assert (y == -float("inf")).all()
+
+
+# ----------------------------------------------------------- gelu's negative tail
+def gelu64(x, dtype):
+    """f and its bound, 16 units of 2^-24 of itself: e 2^n to 4 of them (the exponent's
+    parts, exp2), the scaled tail to 10, two products; in 16 bits the rounding of the
+    exponent x^2 / 2 too."""
+    f = x * 0.5 * torch.special.erfc(torch.as_tensor(-x / np.sqrt(2))).numpy()
+    return f, (16 + (0 if dtype == torch.float32 else 1) * x * x / 2) * ref.U32 * np.abs(f)
+
+
+def gelu_slope64(x, dtype):
+    """f' and its bound, as many units of what is added up."""
+    cdf = 0.5 * torch.special.erfc(torch.as_tensor(-x / np.sqrt(2))).numpy()
+    pdf = np.exp(-0.5 * x * x) / np.sqrt(2 * np.pi)
+    units = 16 + (0 if dtype == torch.float32 else 1) * x * x / 2
+    return cdf + x * pdf, units * ref.U32 * (cdf + np.abs(x) * pdf)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gelu_tail(dtype):
+    """Every value down to where 32 bits hold none, and its slope, as good relatively
+    as it is near 0."""
+    x = np.concatenate([np.linspace(-14, 6, 20001), [-13.9, -5.5, -5.0, 12.0, 30.0, 1000.0, -20.0, -1000.0]])
+    x = ref.f64(dev(x, dtype)).reshape(-1, 1)
+    y, p = lsmgnn.act8(dev(x, dtype), "gelu")
+    f, bf = gelu64(x, dtype)
+    ref.assert_within(y, f, bf + LEAST, dtype, "y")
+    kept = ref.pack(x)[2]
+    df, bdf = gelu_slope64(kept, dtype)
+    dx = lsmgnn.act8_grad(torch.ones_like(y), p, "gelu")
+    ref.assert_within(dx, df, bdf + LEAST, dtype, "dx")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gelu_with_large_and_small_factors(dtype):
+    check_far(dtype, "gelu", lambda x: gelu64(x, dtype), lambda x: gelu_slope64(x, dtype))
