@@ -129,7 +129,9 @@ __device__ __forceinline__ void keep8(const float (&v)[kLane], const Place &p, i
   if (p.col % kPack == 0) *scale = (uint8_t)byte;
 }
 
-// The kept values.  Scale 255 is 2^128, infinity, and its q are 0: NaN.
+// The kept values.  Scale 255 is 2^128, infinity, and its q are 0: NaN.  kFinite: a value
+// of 2^128 is the largest float instead of an infinity, whose slope would be a NaN.
+template <bool kFinite = false>
 __device__ __forceinline__ void kept8(const int8_t *q, const uint8_t *scale, int count, float (&v)[kLane]) {
   const float unit = __uint_as_float(count ? (uint32_t)*scale << 23 : 0);
   int8_t t[kLane];
@@ -141,6 +143,9 @@ __device__ __forceinline__ void kept8(const int8_t *q, const uint8_t *scale, int
   }
 #pragma unroll
   for (int e = 0; e < kLane; ++e) v[e] = (float)t[e] * unit;
+  if (kFinite && unit == 0x1p122f)  // 64 of them are 2^128
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) v[e] = fminf(fmaxf(v[e], -0x1.fffffep127f), 0x1.fffffep127f);
 }
 
 // exp(-a) = e 2^n for 0 <= a <= 800, e to about the last bit in [0.7, 1.5]: a log2(e) in
@@ -304,8 +309,8 @@ __global__ __launch_bounds__(kBlock) void k_act_grad(Cut c, const T *dy, uint64_
     const int8_t *qp = q + p[u].row * kRows * c.dim + p[u].col;
     const uint8_t *sp = scale + p[u].row * kRows * c.nb + p[u].block;
     load8(dy + p[u].row * dyld + p[u].col, p[u].count, g[u]);
-    kept8(qp, sp, p[u].count, a[u]);
-    if (kGated) kept8(qp + c.dim, sp + c.nb, p[u].count, b[u]);
+    kept8<true>(qp, sp, p[u].count, a[u]);
+    if (kGated) kept8<true>(qp + c.dim, sp + c.nb, p[u].count, b[u]);
   }
 #pragma unroll
   for (int u = 0; u < kGradPlaces; ++u) {

@@ -125,3 +125,34 @@ def test_gelu_tail(dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_gelu_with_large_and_small_factors(dtype):
     check_far(dtype, "gelu", lambda x: gelu64(x, dtype), lambda x: gelu_slope64(x, dtype))
+
+
+# ------------------------------------------------- values kept as a power too large
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradient_of_the_largest_numbers(dtype, act):
+    """The largest numbers are kept as 2^128, which 32 bits hold as an infinity only;
+    their gradients are those of 2^128 all the same."""
+    big = torch.finfo(dtype).max
+    x = torch.tensor([[big, 0.5], [-big, 0.5], [1.0, big], [1.0, -big], [-3.0, big]], device="cuda").to(dtype)
+    dy = torch.full((5, 1), 0.25, device="cuda").to(dtype)
+    both = ref.pack(ref.f64(x).reshape(-1, 1))[2].reshape(5, 2)
+    a, b, g = both[:, :1], both[:, 1:], ref.f64(dy)
+    assert np.abs(both).max() == 2.0 ** 128
+    _, p = lsmgnn.act8(x, act, True)
+    f, df = (v.numpy() for v in f64_of(act, torch.as_tensor(a)))
+    dx = lsmgnn.act8_grad(dy, p, act, True)
+    # 20 units of 2^-24: 16 for f and f', 2^128 as the float below it, the products
+    want = np.concatenate([g * b * df, g * f], 1)
+    ref.assert_within(dx, want, 20 * ref.U32 * (np.abs(want) + np.concatenate([np.abs(g * b), 0 * g], 1)), dtype)
+    _, p = lsmgnn.act8(x[:2, :1].contiguous(), act)
+    ref.assert_within(lsmgnn.act8_grad(dy[:2], p, act), (g * df)[:2], 20 * ref.U32, dtype)
+
+
+def f64_of(act, x):
+    """f and f' in 64 bits where x may be very large."""
+    if act == "silu":
+        p, q = torch.sigmoid(x), torch.sigmoid(-x)
+        return x * p, p * (1 + x * q)
+    cdf = 0.5 * torch.special.erfc(-x / 2 ** 0.5)
+    return x * cdf, cdf + x * torch.exp(-0.5 * x * x) / (2 * np.pi) ** 0.5
