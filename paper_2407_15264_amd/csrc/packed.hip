@@ -1019,12 +1019,12 @@ lsmgnn_status lsmgnn_weight_grad8(const int8_t *q, const uint8_t *scale, uint64_
   p.din = (uint32_t)din;
   p.dout = (uint32_t)dout;
   p.nb = (uint32_t)lsmgnn_pack_blocks(din);
-  p.dy_ld = dy_ld;
+  p.dy_ld = rows > 1 ? dy_ld : dout;  // the rows past the last are told by it
   p.offsets = offsets;
   p.experts = num_experts;
   Shape s = shape_of(rows, din, dout);
   // fewer than 4 columns of x or 2 of dy, or 64 rows of dy beyond 32-bit offsets
-  const bool any = din < 4 || dout < 2 || dy_ld > (1u << 23);
+  const bool any = din < 4 || dout < 2 || p.dy_ld > (1u << 23);
   if (any) {
     s.m = s.n = 64;
     s.tiles_m = (uint32_t)blocks_for(din, 64);

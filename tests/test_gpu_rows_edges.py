@@ -156,3 +156,22 @@ def f64_of(act, x):
         return x * p, p * (1 + x * q)
     cdf = 0.5 * torch.special.erfc(-x / 2 ** 0.5)
     return x * cdf, cdf + x * torch.exp(-0.5 * x * x) / (2 * np.pi) ** 0.5
+
+
+# --------------------------------------------------- the weight gradient's row of dy
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("ld", [0, 1, 70])
+def test_weight_gradient_of_one_row_whatever_its_stride(dtype, ld):
+    """A single row has no next one: its stride says nothing, and no element of dy
+    counts twice."""
+    dout = 70
+    x = torch.tensor([[0.5, -0.25, 1.0, 0.125, -0.5]], device="cuda").to(dtype)
+    dy = torch.ones((1, dout), device="cuda").to(dtype)
+    dy[0, 3], dy[0, 40] = float("inf"), -float("inf")
+    p = lsmgnn.pack8(x)
+    dw = torch.empty((5, dout), device="cuda")
+    code = lsmgnn.ELEMENT_TYPES[ref.name_of(dtype)]
+    rc = lsmgnn.lib().lsmgnn_weight_grad8(p.q.data_ptr(), p.scale.data_ptr(), 1, 5, dy.data_ptr(), dout, ld, code, None,
+                                          1, dw.data_ptr(), 0, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == lsmgnn.OK
+    assert np.array_equal(ref.f64(dw), ref.f64(x).T * ref.f64(dy))
