@@ -553,7 +553,8 @@ lsmgnn_status lsmgnn_act8_grad(const void *dy, uint64_t rows, uint64_t dim, uint
    ascending, within [0, rows] (those of a plan; entries out of order or range are
    read as the nearest that are not), or NULL for one expert with all rows.
    dw is num_experts * din rows of dout elements without gaps.  The products are
-   exact; the sums are in 32 bits. */
+   exact, but of elements of a float32 dy below 2^-110, which count to within
+   2^-133; the sums are in 32 bits. */
 uint64_t lsmgnn_weight_grad8_work_bytes(uint64_t rows, uint64_t din, uint64_t dout, uint32_t num_experts);
 lsmgnn_status lsmgnn_weight_grad8(const int8_t *q, const uint8_t *scale, uint64_t rows, uint64_t din, const void *dy,
                                   uint64_t dout, uint64_t dy_ld, uint32_t dy_type, const int32_t *offsets,

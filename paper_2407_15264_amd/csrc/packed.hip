@@ -348,7 +348,7 @@ uint64_t blocks_of(const Cut &c, int per = 1) { return blocks_for(c.rows * c.nb 
 // dw[e] = sum over the expert's rows of x^T dy, on the bfloat16 matrix units with
 // 32-bit sums.  The kept values are exact in bfloat16; dy is one bfloat16, or the
 // sum of two (float16) or three (float32), each multiplied by itself, so that every
-// product is exact.
+// product is exact; the three end at 2^-133, a bfloat16's least.
 //
 // A block computes a tile of dw[e] over kc consecutive rows of the expert; an
 // expert with more rows has its partial sums added, in order, by a second kernel.

@@ -175,3 +175,20 @@ def test_weight_gradient_of_one_row_whatever_its_stride(dtype, ld):
                                           1, dw.data_ptr(), 0, None, 0, torch.cuda.current_stream().cuda_stream)
     assert rc == lsmgnn.OK
     assert np.array_equal(ref.f64(dw), ref.f64(x).T * ref.f64(dy))
+
+
+@pytest.mark.parametrize("power", [-60, -90, -100, -105, -110, -115, -120, -126, -130])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weight_gradient_of_small_numbers(dtype, power):
+    """A float32 dy is three bfloat16 numbers, whose least is 2^-133: its elements count
+    to within that."""
+    rng = np.random.default_rng(-power)
+    x = rng.integers(-100, 101, (200, 8)).astype(np.float64)
+    x[:, 0] = 127
+    dy = rng.standard_normal((200, 6)) * 2.0 ** power
+    x, dy = dev(x, torch.float32), dev(dy, dtype)
+    p = lsmgnn.pack8(x)
+    v, g = ref.f64(lsmgnn.unpack8(p, torch.float32)), ref.f64(dy)
+    got = lsmgnn.weight_grad8(p, dy)[0]
+    size = np.abs(v).T @ (np.abs(g) * 202 * ref.U32 + (2.0 ** -133 if dtype == torch.float32 else 0.0))
+    ref.assert_within(got, v.T @ g, size, torch.float32)
