@@ -423,8 +423,9 @@ lsmgnn_status lsmgnn_split_by_type_noalloc_async(const int64_t *ids, uint64_t n,
    of the element types below, whose starts are `ld` elements apart (ld >= dim
    where there is more than one row; ld <= 2^32), at any address that is a
    multiple of the element's size; rows < 2^31 and rows * dim <= 2^33, but for a
-   table and the whole gradient of one.  No output may overlap an input.  Every call
-   queues its work on `stream` and returns; none allocates, none waits for the
+   table and the whole gradient of one.  No output may overlap an input.  All memory
+   is of one device, that of `stream` (with NULL, the default stream, the device that
+   is current).  Every call queues its work on `stream` and returns; none allocates, none waits for the
    device and each can be captured in a HIP graph.  Where a call takes `work`,
    that is device memory of the caller's, 256-byte aligned, of at least the
    bytes its _work_bytes function names, free again once the stream has run the

@@ -907,6 +907,8 @@ lsmgnn_status lsmgnn_embed_rows(const void *table, uint64_t num_rows, uint64_t d
       !matrix_ok(out, n, dim, out_ld, out_type) || (n && !ids) || !status_view(status, &st_word))
     return LSMGNN_E_INVAL;
   if (n == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(table_type, [&](auto ti) {
     with_type(out_type, [&](auto to) {
@@ -942,6 +944,8 @@ lsmgnn_status lsmgnn_embed_grad(const void *dy, uint64_t dim, uint64_t dy_ld, ui
                              work_bytes) ||
       !status_view(status, &st_word))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const uint32_t es = elem_bytes(grad_type);
   Sums s{};
@@ -989,6 +993,8 @@ lsmgnn_status lsmgnn_embed_grad_rows(const void *dy, uint64_t dim, uint64_t dy_l
                                     work_bytes) ||
       (n && !unique) || !status_view(result_host, &res))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n) {
     const Plan p = plan_of(n, num_rows, dim, 16 / elem_bytes(dy_type));

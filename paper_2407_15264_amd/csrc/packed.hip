@@ -929,6 +929,8 @@ lsmgnn_status lsmgnn_pack8(const void *x, uint64_t rows, uint64_t dim, uint64_t 
   using namespace lsm_packed;
   if (!matrix_ok(x, rows, dim, x_ld, type) || !kept_ok(q, scale, rows, dim)) return LSMGNN_E_INVAL;
   if (rows == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -943,6 +945,8 @@ lsmgnn_status lsmgnn_unpack8(const int8_t *q, const uint8_t *scale, uint64_t row
   using namespace lsm_packed;
   if (!matrix_ok(out, rows, dim, out_ld, type) || !kept_ok(q, scale, rows, dim)) return LSMGNN_E_INVAL;
   if (rows == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -959,6 +963,8 @@ lsmgnn_status lsmgnn_act8(const void *x, uint64_t rows, uint64_t dim, uint64_t x
       !matrix_ok(y, rows, dim, y_ld, type) || !kept_ok(q, scale, rows * (1 + gated), dim))
     return LSMGNN_E_INVAL;
   if (rows == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -980,6 +986,8 @@ lsmgnn_status lsmgnn_act8_grad(const void *dy, uint64_t rows, uint64_t dim, uint
       !matrix_ok(dx, rows, dim * (1 + gated), dx_ld, type) || !kept_ok(q, scale, rows * (1 + gated), dim))
     return LSMGNN_E_INVAL;
   if (rows == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -1011,6 +1019,8 @@ lsmgnn_status lsmgnn_weight_grad8(const int8_t *q, const uint8_t *scale, uint64_
       !matrix_ok(dw, num_experts * din, dout, dout, dw_type) ||
       (need && (!work || reinterpret_cast<uintptr_t>(work) % 256 || work_bytes < need)))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   Products p{};
   p.q = q;

@@ -293,6 +293,8 @@ lsmgnn_status lsmgnn_route_plan(const int64_t *experts, uint64_t n, uint32_t k, 
       (need && (!work || reinterpret_cast<uintptr_t>(work) % 256 || work_bytes < need)) ||
       !status_view(status, &st_word))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const ToPlan to{offsets, slot, source, num_experts, (uint32_t)rows, st_word};
   if (n) {
@@ -314,6 +316,8 @@ lsmgnn_status lsmgnn_route_rows(const void *x, uint64_t n, uint64_t dim, uint64_
   if (!choices_ok(n, k) || !matrix_ok(x, n, dim, x_ld, type) || !matrix_ok(out, rows, dim, out_ld, type) ||
       (n && !slot) || (rows && !source))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -338,6 +342,8 @@ lsmgnn_status lsmgnn_route_combine(const void *z, uint64_t rows, uint64_t dim, u
       (n && !slot))
     return LSMGNN_E_INVAL;
   if (n == 0) return LSMGNN_OK;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
@@ -356,6 +362,8 @@ lsmgnn_status lsmgnn_route_combine_grad(const void *dy, uint64_t n, uint64_t dim
   if (!choices_ok(n, k) || !matrix_ok(dy, n, dim, dy_ld, type) || !matrix_ok(dz, rows, dim, dz_ld, type) ||
       (n && !slot) || (rows && !source) || (dweights && (!weights || !matrix_ok(z, rows, dim, z_ld, type))))
     return LSMGNN_E_INVAL;
+  const StreamDevice on(stream);
+  if (!on.ok) return LSMGNN_E_DEVICE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;

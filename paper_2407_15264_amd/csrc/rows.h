@@ -79,6 +79,26 @@ inline bool status_view(uint64_t *p, uint64_t **out) {
   return true;
 }
 
+// Makes the device of a caller's stream the current one; the NULL stream is the
+// current device's already.
+struct StreamDevice {
+  int prev = -1;
+  bool ok = true;
+  explicit StreamDevice(void *stream) {
+    int dev = -1, now = -1;
+    if (!stream) return;
+    ok = hipStreamGetDevice(static_cast<hipStream_t>(stream), &dev) == hipSuccess && hipGetDevice(&now) == hipSuccess;
+    if (ok && dev != now) {
+      ok = hipSetDevice(dev) == hipSuccess;
+      if (ok) prev = now;
+    }
+    if (!ok) (void)hipGetLastError();
+  }
+  ~StreamDevice() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
+
 // kN elements at p, which may be any address: rows of an odd width start anywhere,
 // and the hardware takes vector accesses so.  Whole vectors (a copy of the elements
 // would be taken apart by the compiler where another path reads some of them).

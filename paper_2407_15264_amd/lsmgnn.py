@@ -601,19 +601,34 @@ def _vector(t, dtype, numel, name, device):
     return t.data_ptr()
 
 
-_raw_stream = None
+_raw_stream = _raw_device = None
 
 
-def _stream_of(stream, device):
-    """The hipStream_t of `stream`, or of the current one (looked up without
-    making a Stream object: 0.1 us against 2)."""
-    global _raw_stream
-    if stream is not None:
-        return stream.cuda_stream
+def _run(name, device, stream, *args):
+    """Call the library's `name` on `stream` (None: the current one of `device`, the
+    tensors' device) with that device current: the handle of a default stream, 0, is
+    the current device's.  Looked up without making a Stream object: 0.1 us against
+    2."""
+    global _raw_stream, _raw_device
     if _raw_stream is None:
         import torch
-        _raw_stream = torch._C._cuda_getCurrentRawStream
-    return _raw_stream(device.index)
+        _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    index = device.index
+    if stream is None:
+        handle = _raw_stream(index)
+    else:
+        if stream.device != device:
+            raise ValueError(f"stream is of {stream.device}, not of {device}")
+        handle = stream.cuda_stream
+    fn = getattr(lib(), name)
+    if _raw_device() == index:
+        rc = fn(*args, handle)
+    else:
+        import torch
+        with torch.cuda.device(device):
+            rc = fn(*args, handle)
+    if rc:
+        _check(rc, name)
 
 
 def _empty(shape, dtype, device, stream):
@@ -643,6 +658,8 @@ def _work(nbytes, work, device, stream):
         import torch
         work = _empty(nbytes, torch.uint8, device, stream)
     _dev_ptr(work, work.dtype, "work")
+    if work.device != device:
+        raise ValueError(f"work is on {work.device}, not on {device}")
     return work, work.data_ptr(), work.numel() * work.element_size()
 
 
@@ -659,8 +676,8 @@ def embed_rows(table, ids, scale=1.0, pad=None, dtype=None, out=None, status_ptr
     n = ids.numel()
     ip = _vector(ids, torch.int64, n, "ids", device)
     out, op, old, ot = _output(out, "out", n, dim, dtype or table.dtype, device, stream)
-    _check(lib().lsmgnn_embed_rows(tp, num_rows, dim, tld, tt, ip, n, NO_PAD if pad is None else pad, scale, op, old,
-                                   ot, status_ptr, _stream_of(stream, device)), "lsmgnn_embed_rows")
+    _run("lsmgnn_embed_rows", device, stream, tp, num_rows, dim, tld, tt, ip, n, NO_PAD if pad is None else pad,
+         scale, op, old, ot, status_ptr)
     return out
 
 
@@ -680,8 +697,8 @@ def embed_grad(dy, ids, num_rows, scale=1.0, pad=None, dtype=None, grad=None, wo
     ip = _vector(ids, torch.int64, n, "ids", device)
     grad, gp, gld, gt = _output(grad, "grad", num_rows, dim, dtype or dy.dtype, device, stream)
     work, wp, wb = _work(embed_grad_work_bytes(n, num_rows, dim), work, device, stream)
-    _check(lib().lsmgnn_embed_grad(dp, dim, dld, dt, ip, n, num_rows, NO_PAD if pad is None else pad, scale, gp, gld,
-                                   gt, wp, wb, status_ptr, _stream_of(stream, device)), "lsmgnn_embed_grad")
+    _run("lsmgnn_embed_grad", device, stream, dp, dim, dld, dt, ip, n, num_rows, NO_PAD if pad is None else pad,
+         scale, gp, gld, gt, wp, wb, status_ptr)
     return grad
 
 
@@ -697,9 +714,8 @@ def embed_grad_rows_async(dy, ids, num_rows, unique, rows, result_ptr, scale=1.0
     up = _vector(unique, torch.int64, n, "unique", device)
     rp, _, _, rld, rt = _matrix(rows, "rows", dim, n, device)
     work, wp, wb = _work(embed_grad_work_bytes(n, num_rows, dim), work, device, stream)
-    _check(lib().lsmgnn_embed_grad_rows(dp, dim, dld, dt, ip, n, num_rows, NO_PAD if pad is None else pad, scale, up,
-                                        rp, rld, rt, wp, wb, result_ptr, _stream_of(stream, device)),
-           "lsmgnn_embed_grad_rows")
+    _run("lsmgnn_embed_grad_rows", device, stream, dp, dim, dld, dt, ip, n, num_rows, NO_PAD if pad is None else pad,
+         scale, up, rp, rld, rt, wp, wb, result_ptr)
 
 
 def embed_grad_rows(dy, ids, num_rows, scale=1.0, pad=None, dtype=None, work=None, stream=None):
@@ -770,8 +786,7 @@ def route_plan(experts, num_experts, align=1, work=None, status_ptr=None, stream
         raise ValueError("too many sorted rows")
     plan = RoutePlan(n, k, num_experts, align, rows, device, stream)
     work, wp, wb = _work(L.lsmgnn_route_work_bytes(n, k, num_experts), work, device, stream)
-    _check(L.lsmgnn_route_plan(ep, n, k, num_experts, align, *plan._ptrs(), wp, wb, status_ptr,
-                               _stream_of(stream, device)), "lsmgnn_route_plan")
+    _run("lsmgnn_route_plan", device, stream, ep, n, k, num_experts, align, *plan._ptrs(), wp, wb, status_ptr)
     return plan
 
 
@@ -783,8 +798,7 @@ def route_rows(x, plan, out=None, stream=None):
     out, op, old, ot = _output(out, "out", plan.rows, dim, x.dtype, device, stream)
     if ot != xt:
         raise TypeError("x and out must have one type")
-    _check(lib().lsmgnn_route_rows(xp, n, dim, xld, xt, *plan._ptrs()[1:], plan.k,
-                                   plan.rows, op, old, _stream_of(stream, device)), "lsmgnn_route_rows")
+    _run("lsmgnn_route_rows", device, stream, xp, n, dim, xld, xt, *plan._ptrs()[1:], plan.k, plan.rows, op, old)
     return out
 
 
@@ -799,8 +813,7 @@ def route_combine(z, plan, weights=None, out=None, stream=None):
     out, op, old, ot = _output(out, "out", plan.n, dim, z.dtype, device, stream)
     if ot != zt:
         raise TypeError("z and out must have one type")
-    _check(lib().lsmgnn_route_combine(zp, rows, dim, zld, zt, plan._ptrs()[1], wp, plan.n, plan.k, op, old,
-                                      _stream_of(stream, device)), "lsmgnn_route_combine")
+    _run("lsmgnn_route_combine", device, stream, zp, rows, dim, zld, zt, plan._ptrs()[1], wp, plan.n, plan.k, op, old)
     return out
 
 
@@ -816,9 +829,8 @@ def route_combine_grad(dy, z, plan, weights, dz=None, stream=None):
     if zt != dt or ot != dt:
         raise TypeError("dy, z and dz must have one type")
     dw = _empty((plan.n, plan.k), torch.float32, device, stream)
-    _check(lib().lsmgnn_route_combine_grad(dp, n, dim, dld, dt, zp, zld, *plan._ptrs()[1:],
-                                           wp, plan.k, rows, op, old, dw.data_ptr(), _stream_of(stream, device)),
-           "lsmgnn_route_combine_grad")
+    _run("lsmgnn_route_combine_grad", device, stream, dp, n, dim, dld, dt, zp, zld, *plan._ptrs()[1:], wp, plan.k,
+         rows, op, old, dw.data_ptr())
     return dz, dw
 
 
@@ -867,7 +879,7 @@ def pack8(x, packed=None, stream=None):
     xp, rows, dim, ld, t = _matrix(x, "x")
     packed = packed or Packed8(rows, dim, device, stream)
     qp, sp = packed._ptrs(rows, dim, device)
-    _check(lib().lsmgnn_pack8(xp, rows, dim, ld, t, qp, sp, _stream_of(stream, device)), "lsmgnn_pack8")
+    _run("lsmgnn_pack8", device, stream, xp, rows, dim, ld, t, qp, sp)
     return packed
 
 
@@ -878,7 +890,7 @@ def unpack8(packed, dtype=None, out=None, stream=None):
     device, rows, dim = packed.device, packed.rows, packed.dim
     out, op, ld, t = _output(out, "out", rows, dim, dtype or torch.bfloat16, device, stream)
     qp, sp = packed._ptrs(rows, dim, device)
-    _check(lib().lsmgnn_unpack8(qp, sp, rows, dim, op, ld, t, _stream_of(stream, device)), "lsmgnn_unpack8")
+    _run("lsmgnn_unpack8", device, stream, qp, sp, rows, dim, op, ld, t)
     return out
 
 
@@ -897,8 +909,7 @@ def act8(x, act, gated=False, out=None, packed=None, stream=None):
         raise TypeError("x and out must have one type")
     packed = packed or Packed8(rows * parts, dim, device, stream)
     qp, sp = packed._ptrs(rows * parts, dim, device)
-    _check(lib().lsmgnn_act8(xp, rows, dim, ld, t, code, parts - 1, yp, yld, qp, sp, _stream_of(stream, device)),
-           "lsmgnn_act8")
+    _run("lsmgnn_act8", device, stream, xp, rows, dim, ld, t, code, parts - 1, yp, yld, qp, sp)
     return out, packed
 
 
@@ -912,8 +923,7 @@ def act8_grad(dy, packed, act, gated=False, dx=None, stream=None):
     if xt != t:
         raise TypeError("dy and dx must have one type")
     qp, sp = packed._ptrs(rows * parts, dim, device)
-    _check(lib().lsmgnn_act8_grad(dp, rows, dim, dld, t, qp, sp, code, parts - 1, xp, xld,
-                                  _stream_of(stream, device)), "lsmgnn_act8_grad")
+    _run("lsmgnn_act8_grad", device, stream, dp, rows, dim, dld, t, qp, sp, code, parts - 1, xp, xld)
     return dx
 
 
@@ -939,7 +949,6 @@ def weight_grad8(packed, dy, offsets=None, dtype=None, out=None, work=None, stre
         out = _empty((experts, din, dout), dtype or torch.float32, device, stream)
     op = _vector(out, out.dtype, experts * din * dout, "out", device)
     work, wp, wb = _work(weight_grad8_work_bytes(rows, din, dout, experts), work, device, stream)
-    _check(lib().lsmgnn_weight_grad8(qp, sp, rows, din, dp, dout, dld, dt, fp, experts, op,
-                                     _type_code(out.dtype, "out"), wp, wb, _stream_of(stream, device)),
-           "lsmgnn_weight_grad8")
+    _run("lsmgnn_weight_grad8", device, stream, qp, sp, rows, din, dp, dout, dld, dt, fp, experts, op,
+         _type_code(out.dtype, "out"), wp, wb)
     return out
