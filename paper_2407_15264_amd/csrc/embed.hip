@@ -970,6 +970,11 @@ lsmgnn_status lsmgnn_embed_grad(const void *dy, uint64_t dim, uint64_t dy_ld, ui
     else
       hipLaunchKernelGGL(k_zero_rows<uint16_t>, dim3(num_rows < 8192 ? num_rows : 8192), dim3(kBlock), 0, st,
                          static_cast<uint16_t *>(grad), num_rows, dim, grad_ld);
+    constexpr uint64_t kMostFill = 1ull << 36;  // 2^30 lanes
+    for (; zeros.bytes > kMostFill; zeros = lsm_sort::Fill::of(zeros.at + kMostFill, zeros.bytes - kMostFill)) {
+      const lsm_sort::Fill some = lsm_sort::Fill::of(zeros.at, kMostFill);
+      hipLaunchKernelGGL(k_fill, dim3(some.blocks(kBlock)), dim3(kBlock), 0, st, some);
+    }
     if (n) {
       const Plan p = plan_of(n, num_rows, dim, 16 / elem_bytes(dy_type));
       uint8_t *w = static_cast<uint8_t *>(work);

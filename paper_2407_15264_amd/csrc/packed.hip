@@ -344,6 +344,12 @@ Cut cut_of(uint64_t rows, uint64_t dim) {
 
 uint64_t blocks_of(const Cut &c, int per = 1) { return blocks_for(c.rows * c.nb * kQuads, kBlock * per); }
 
+// f(cut, first row) for launches of all rows.
+template <typename F>
+void cuts_of(uint64_t rows, uint64_t dim, F f) {
+  in_launches(rows, blocks_for(dim, kPack) * kQuads, [&](uint64_t r, uint64_t n) { f(cut_of(n, dim), r); });
+}
+
 // ------------------------------------------------------------ weight gradient
 // dw[e] = sum over the expert's rows of x^T dy, on the bfloat16 matrix units with
 // 32-bit sums.  The kept values are exact in bfloat16; dy is one bfloat16, or the
@@ -931,11 +937,12 @@ lsmgnn_status lsmgnn_pack8(const void *x, uint64_t rows, uint64_t dim, uint64_t 
   if (rows == 0) return LSMGNN_OK;
   const StreamDevice on(stream);
   if (!on.ok) return LSMGNN_E_DEVICE;
-  const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
-    hipLaunchKernelGGL((k_pack<T>), dim3(blocks_of(c)), dim3(kBlock), 0, static_cast<hipStream_t>(stream), c,
-                       static_cast<const T *>(x), x_ld, q, scale);
+    cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
+      hipLaunchKernelGGL((k_pack<T>), dim3(blocks_of(c)), dim3(kBlock), 0, static_cast<hipStream_t>(stream), c,
+                         static_cast<const T *>(x) + r * x_ld, x_ld, q + r * dim, scale + r * c.nb);
+    });
   });
   return done();
 }
@@ -947,11 +954,12 @@ lsmgnn_status lsmgnn_unpack8(const int8_t *q, const uint8_t *scale, uint64_t row
   if (rows == 0) return LSMGNN_OK;
   const StreamDevice on(stream);
   if (!on.ok) return LSMGNN_E_DEVICE;
-  const Cut c = cut_of(rows, dim);
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
-    hipLaunchKernelGGL((k_unpack<T>), dim3(blocks_of(c)), dim3(kBlock), 0, static_cast<hipStream_t>(stream), c, q,
-                       scale, static_cast<T *>(out), out_ld);
+    cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
+      hipLaunchKernelGGL((k_unpack<T>), dim3(blocks_of(c)), dim3(kBlock), 0, static_cast<hipStream_t>(stream), c,
+                         q + r * dim, scale + r * c.nb, static_cast<T *>(out) + r * out_ld, out_ld);
+    });
   });
   return done();
 }
@@ -965,14 +973,15 @@ lsmgnn_status lsmgnn_act8(const void *x, uint64_t rows, uint64_t dim, uint64_t x
   if (rows == 0) return LSMGNN_OK;
   const StreamDevice on(stream);
   if (!on.ok) return LSMGNN_E_DEVICE;
-  const Cut c = cut_of(rows, dim);
+  const uint64_t kept = 1 + gated;  // kept rows of a row
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
     with_act(act, gated, [&](auto f, auto g) {
-      hipLaunchKernelGGL((k_act<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kActPlaces)),
-                         dim3(kBlock), 0,
-                         static_cast<hipStream_t>(stream), c, static_cast<const T *>(x), x_ld, static_cast<T *>(y),
-                         y_ld, q, scale);
+      cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
+        hipLaunchKernelGGL((k_act<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kActPlaces)),
+                           dim3(kBlock), 0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(x) + r * x_ld,
+                           x_ld, static_cast<T *>(y) + r * y_ld, y_ld, q + r * kept * dim, scale + r * kept * c.nb);
+      });
     });
   });
   return done();
@@ -988,14 +997,15 @@ lsmgnn_status lsmgnn_act8_grad(const void *dy, uint64_t rows, uint64_t dim, uint
   if (rows == 0) return LSMGNN_OK;
   const StreamDevice on(stream);
   if (!on.ok) return LSMGNN_E_DEVICE;
-  const Cut c = cut_of(rows, dim);
+  const uint64_t kept = 1 + gated;  // kept rows of a row
   with_type(type, [&](auto tag) {
     typedef typename decltype(tag)::T T;
     with_act(act, gated, [&](auto f, auto g) {
-      hipLaunchKernelGGL((k_act_grad<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kGradPlaces)),
-                         dim3(kBlock), 0,
-                         static_cast<hipStream_t>(stream), c, static_cast<const T *>(dy), dy_ld, q, scale,
-                         static_cast<T *>(dx), dx_ld);
+      cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
+        hipLaunchKernelGGL((k_act_grad<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kGradPlaces)),
+                           dim3(kBlock), 0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(dy) + r * dy_ld,
+                           dy_ld, q + r * kept * dim, scale + r * kept * c.nb, static_cast<T *>(dx) + r * dx_ld, dx_ld);
+      });
     });
   });
   return done();

@@ -370,11 +370,16 @@ lsmgnn_status lsmgnn_route_combine_grad(const void *dy, uint64_t n, uint64_t dim
     const uint32_t np = pieces(dim, kPiece<T>);
     uint32_t shift = 0;
     while (shift < 6 && (1u << shift) < np) ++shift;
-    const uint64_t move = blocks_for(n, kBlock >> shift), grid = move + blocks_for(rows, kBlock);
-    if (grid)
-      hipLaunchKernelGGL((k_route_combine_grad<T>), dim3(grid), dim3(kBlock), 0, st, n, (uint32_t)dim,
-                         static_cast<const T *>(dy), dy_ld, static_cast<const T *>(z), z_ld, slot, weights, k, shift,
-                         move, source, rows, static_cast<T *>(dz), dz_ld, dweights);
+    auto launch = [&](uint64_t t, uint64_t tokens, bool unused) {
+      const uint64_t move = blocks_for(tokens, kBlock >> shift), grid = move + (unused ? blocks_for(rows, kBlock) : 0);
+      hipLaunchKernelGGL((k_route_combine_grad<T>), dim3(grid), dim3(kBlock), 0, st, tokens, (uint32_t)dim,
+                         static_cast<const T *>(dy) + t * dy_ld, dy_ld, static_cast<const T *>(z), z_ld, slot + t * k,
+                         weights ? weights + t * k : nullptr, k, shift, move, source, rows, static_cast<T *>(dz), dz_ld,
+                         dweights ? dweights + t * k : nullptr);
+    };
+    // the unused rows beside the first tokens
+    in_launches(n, 1u << shift, [&](uint64_t t, uint64_t tokens) { launch(t, tokens, t == 0); });
+    if (n == 0 && rows) launch(0, 0, true);
   });
   return hipGetLastError() == hipSuccess ? LSMGNN_OK : LSMGNN_E_DEVICE;
 }

@@ -13,8 +13,8 @@ namespace lsm_rows {
 constexpr int kBlock = 256;
 constexpr uint64_t kMaxDim = 65536;             // elements of a row
 constexpr uint64_t kMaxRows = (1ull << 31) - 1;  // rows or places that a 32-bit index names
-// elements of a matrix that a launch covers: a lane takes a 16-byte piece, and a
-// launch has fewer than 2^32 lanes
+// elements of a matrix: where a row's lanes take a 16-byte piece each and no row has
+// spare ones, a launch has fewer than 2^32 lanes, as it must
 constexpr uint64_t kMaxElems = 1ull << 33;
 
 template <uint32_t kType>
@@ -59,7 +59,7 @@ inline bool ld_ok(const void *p, uint64_t rows, uint64_t dim, uint64_t ld, uint3
          (rows == 0 || p) && reinterpret_cast<uintptr_t>(p) % elem_bytes(type) == 0;
 }
 
-// The same for a matrix that a launch covers.
+// The same for a matrix of bounded size.
 inline bool matrix_ok(const void *p, uint64_t rows, uint64_t dim, uint64_t ld, uint32_t type) {
   return rows <= kMaxRows && ld_ok(p, rows, dim, ld, type) && rows * dim <= kMaxElems;
 }
@@ -206,6 +206,12 @@ inline uint64_t divider(uint32_t d) { return (1ull << 32) / d + 1; }
 // Blocks for `work` units, `per` of them a block.
 inline uint64_t blocks_for(uint64_t work, uint64_t per) { return (work + per - 1) / per; }
 
-constexpr uint64_t kMaxGrid = 0x7fffffffull;
+// f(first row, rows) for launches of `lanes` lanes a row that have spare ones in narrow
+// rows: at most 2^30 lanes at once.
+template <typename F>
+inline void in_launches(uint64_t rows, uint64_t lanes, F f) {
+  const uint64_t most = (1ull << 30) / lanes;
+  for (uint64_t r = 0; r < rows; r += most) f(r, rows - r < most ? rows - r : most);
+}
 
 }  // namespace lsm_rows

@@ -192,3 +192,49 @@ def test_weight_gradient_of_small_numbers(dtype, power):
     got = lsmgnn.weight_grad8(p, dy)[0]
     size = np.abs(v).T @ (np.abs(g) * 202 * ref.U32 + (2.0 ** -133 if dtype == torch.float32 else 0.0))
     ref.assert_within(got, v.T @ g, size, torch.float32)
+
+
+# ----------------------------------------------------- more lanes than one launch has
+def room_for(gigabytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes << 30:
+        pytest.skip(f"needs {gigabytes} GiB of device memory")
+
+
+def test_kept_rows_of_one_value():
+    """More than 2^30 rows of one value each; whole numbers are kept exactly."""
+    room_for(40)
+    n = (1 << 30) + 77
+    x = torch.randint(-64, 65, (n, 1), dtype=torch.int8, device="cuda").to(torch.bfloat16)
+    p = lsmgnn.pack8(x)
+    assert torch.equal(lsmgnn.unpack8(p), x)
+    del p
+    y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    _, p = lsmgnn.act8(x, "silu", out=y)
+    assert torch.equal(lsmgnn.unpack8(p), x)
+    lsmgnn.act8_grad(x, p, "silu", dx=dx)
+    del p
+    for a in range(0, n, 1 << 27):  # every row was written
+        assert not torch.isnan(y[a:a + (1 << 27)]).any() and not torch.isnan(dx[a:a + (1 << 27)]).any()
+    for a in (0, (1 << 28) - 500, (1 << 29) - 500, (1 << 30) - 500, n - 1000):
+        part = x[a:a + 1000]
+        want, kept = lsmgnn.act8(part, "silu")
+        assert torch.equal(y[a:a + 1000], want)
+        assert torch.equal(dx[a:a + 1000], lsmgnn.act8_grad(part, kept, "silu"))
+
+
+def test_combine_gradient_of_many_tokens():
+    """33 pieces of a row take 64 lanes: 2^32 of them and the unused rows' too."""
+    room_for(100)
+    n, dim = (1 << 33) // 129, 129
+    dy = torch.randint(-100, 100, (n, dim), dtype=torch.int8, device="cuda").float()
+    slot = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    source = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    dz = torch.empty((n, dim), device="cuda")
+    rc = lsmgnn.lib().lsmgnn_route_combine_grad(dy.data_ptr(), n, dim, dim, 0, None, dim, slot.data_ptr(),
+                                                source.data_ptr(), None, 1, n, dz.data_ptr(), dim, None,
+                                                torch.cuda.current_stream().cuda_stream)
+    assert rc == lsmgnn.OK
+    for a in range(0, n, 1 << 23):
+        b = min(n, a + (1 << 23))
+        assert torch.equal(dz[n - b:n - a].flip(0), dy[a:b])
