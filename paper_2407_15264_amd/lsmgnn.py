@@ -571,12 +571,23 @@ def _type_code(dtype, name):
     return code
 
 
+def _no_graph(t, name):
+    """Refuse a tensor whose gradient torch would expect to hear of: the calls below
+    record nothing, and their results would silently end the graph."""
+    import torch
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient, which this call does not record: call it under "
+                           "torch.no_grad() or from a torch.autograd.Function, with the gradient's own call")
+
+
 def _matrix(t, name, dim=None, rows=None, like=None):
     """(address, rows, dim, ld, element type) of a 2-D device tensor whose rows
     are contiguous; with `like`, of the same device."""
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.requires_grad:
+        _no_graph(t, name)
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions, not {t.dim()}")
     n, d = t.shape
@@ -594,6 +605,8 @@ def _matrix(t, name, dim=None, rows=None, like=None):
 def _vector(t, dtype, numel, name, device):
     """Address of a contiguous device tensor of `numel` elements of `dtype`."""
     _dev_ptr(t, dtype, name)
+    if t.requires_grad:
+        _no_graph(t, name)
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, not {t.numel()}")
     if t.device != device:
