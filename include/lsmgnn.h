@@ -460,7 +460,11 @@ lsmgnn_status lsmgnn_embed_rows(const void *table, uint64_t num_rows, uint64_t d
    the distinct IDs in ascending order and rows (n rows) their gradients; once
    the stream has run the call, result_host[0] is how many there are and
    result_host[1] the status (LSMGNN_OK or LSMGNN_E_RANGE), two uint64 in pinned
-   host or device memory; entries past that count are not written.  */
+   host or device memory; entries past that count are not written.
+   lsmgnn_embed_grad takes lsmgnn_table_grad_work_bytes bytes of work, none where
+   one launch does it all; lsmgnn_embed_grad_work_bytes is what
+   lsmgnn_embed_grad_rows takes, and enough for either. */
+uint64_t lsmgnn_table_grad_work_bytes(uint64_t n, uint64_t num_rows, uint64_t dim);
 uint64_t lsmgnn_embed_grad_work_bytes(uint64_t n, uint64_t num_rows, uint64_t dim);
 lsmgnn_status lsmgnn_embed_grad(const void *dy, uint64_t dim, uint64_t dy_ld, uint32_t dy_type, const int64_t *ids,
                                 uint64_t n, uint64_t num_rows, int64_t pad, float scale, void *grad,

@@ -887,11 +887,10 @@ void queue_few_places(Sums s, const void *dy, uint32_t dy_type, const int64_t *i
 
 bool grad_args_ok(const void *dy, uint64_t dim, uint64_t dy_ld, uint32_t dy_type, const int64_t *ids, uint64_t n,
                   uint64_t num_rows, const void *out, uint64_t out_rows, uint64_t out_ld, uint32_t out_type,
-                  const void *work, uint64_t work_bytes) {
+                  const void *work, uint64_t work_bytes, uint64_t need) {
   return num_rows >= 1 && num_rows <= 0xfffffffcull && matrix_ok(dy, n, dim, dy_ld, dy_type) &&
          type_ok(out_type) && ld_ok(out, out_rows, dim, out_ld, out_type) && (n == 0 || ids) &&
-         (n == 0 || (work && reinterpret_cast<uintptr_t>(work) % 256 == 0 &&
-                     work_bytes >= lsmgnn_embed_grad_work_bytes(n, num_rows, dim)));
+         (need == 0 || (work && reinterpret_cast<uintptr_t>(work) % 256 == 0 && work_bytes >= need));
 }
 
 }  // namespace lsm_embed
@@ -934,6 +933,10 @@ uint64_t lsmgnn_embed_grad_work_bytes(uint64_t n, uint64_t num_rows, uint64_t di
   return a > b ? a : b;
 }
 
+uint64_t lsmgnn_table_grad_work_bytes(uint64_t n, uint64_t num_rows, uint64_t dim) {
+  return lsm_embed::few_places(n, num_rows) ? 0 : lsmgnn_embed_grad_work_bytes(n, num_rows, dim);
+}
+
 lsmgnn_status lsmgnn_embed_grad(const void *dy, uint64_t dim, uint64_t dy_ld, uint32_t dy_type, const int64_t *ids,
                                 uint64_t n, uint64_t num_rows, int64_t pad, float scale, void *grad,
                                 uint64_t grad_ld, uint32_t grad_type, void *work, uint64_t work_bytes,
@@ -941,7 +944,7 @@ lsmgnn_status lsmgnn_embed_grad(const void *dy, uint64_t dim, uint64_t dy_ld, ui
   using namespace lsm_embed;
   uint64_t *st_word;
   if (!grad || !grad_args_ok(dy, dim, dy_ld, dy_type, ids, n, num_rows, grad, num_rows, grad_ld, grad_type, work,
-                             work_bytes) ||
+                             work_bytes, lsmgnn_table_grad_work_bytes(n, num_rows, dim)) ||
       !status_view(status, &st_word))
     return LSMGNN_E_INVAL;
   const StreamDevice on(stream);
@@ -995,7 +998,7 @@ lsmgnn_status lsmgnn_embed_grad_rows(const void *dy, uint64_t dim, uint64_t dy_l
   using namespace lsm_embed;
   uint64_t *res;
   if (!result_host || !grad_args_ok(dy, dim, dy_ld, dy_type, ids, n, num_rows, rows, n, rows_ld, rows_type, work,
-                                    work_bytes) ||
+                                    work_bytes, lsmgnn_embed_grad_work_bytes(n, num_rows, dim)) ||
       (n && !unique) || !status_view(result_host, &res))
     return LSMGNN_E_INVAL;
   const StreamDevice on(stream);

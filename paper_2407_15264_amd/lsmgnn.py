@@ -150,6 +150,7 @@ def lib():
         for name, res, args in (
                 ("embed_rows", i32, [vp, u64, u64, u64, u32, vp, u64, i64, f32, vp, u64, u32, vp, vp]),
                 ("embed_grad_work_bytes", u64, [u64, u64, u64]),
+                ("table_grad_work_bytes", u64, [u64, u64, u64]),
                 ("embed_grad", i32, [vp, u64, u64, u32, vp, u64, u64, i64, f32, vp, u64, u32, vp, u64, vp, vp]),
                 ("embed_grad_rows", i32, [vp, u64, u64, u32, vp, u64, u64, i64, f32, vp, vp, u64, u32, vp, u64, vp,
                                           vp]),
@@ -695,8 +696,13 @@ def embed_rows(table, ids, scale=1.0, pad=None, dtype=None, out=None, status_ptr
 
 
 def embed_grad_work_bytes(n, num_rows, dim):
-    """Device work memory the gradient of a lookup of n IDs needs."""
+    """Device work memory the gradient of a lookup of n IDs needs, whole or by rows."""
     return int(lib().lsmgnn_embed_grad_work_bytes(int(n), int(num_rows), int(dim)))
+
+
+def table_grad_work_bytes(n, num_rows, dim):
+    """Device work memory the whole gradient needs: none where one launch does it."""
+    return int(lib().lsmgnn_table_grad_work_bytes(int(n), int(num_rows), int(dim)))
 
 
 def embed_grad(dy, ids, num_rows, scale=1.0, pad=None, dtype=None, grad=None, work=None, status_ptr=None,
@@ -709,7 +715,7 @@ def embed_grad(dy, ids, num_rows, scale=1.0, pad=None, dtype=None, grad=None, wo
     dp, n, dim, dld, dt = _matrix(dy, "dy")
     ip = _vector(ids, torch.int64, n, "ids", device)
     grad, gp, gld, gt = _output(grad, "grad", num_rows, dim, dtype or dy.dtype, device, stream)
-    work, wp, wb = _work(embed_grad_work_bytes(n, num_rows, dim), work, device, stream)
+    work, wp, wb = _work(table_grad_work_bytes(n, num_rows, dim), work, device, stream)
     _run("lsmgnn_embed_grad", device, stream, dp, dim, dld, dt, ip, n, num_rows, NO_PAD if pad is None else pad,
          scale, gp, gld, gt, wp, wb, status_ptr)
     return grad

@@ -46,6 +46,7 @@ def calls(monkeypatch):
 
     fake = types.SimpleNamespace(lsmgnn_route_max_rows=lambda n, k, num, align: n * k,
                                  lsmgnn_route_work_bytes=lambda *a: 256, lsmgnn_embed_grad_work_bytes=lambda *a: 256,
+                                 lsmgnn_table_grad_work_bytes=lambda *a: 256,
                                  lsmgnn_weight_grad8_work_bytes=lambda *a: 256)
     for name in CALLS:
         setattr(fake, "lsmgnn_" + name,
