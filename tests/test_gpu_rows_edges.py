@@ -31,27 +31,28 @@ A_FAR = [-1e30, -1000.0, -400.0, -300.0, -200.0, -104.0, -90.0, -87.0, -50.0, -1
 SIZES = [1e38, 1e36, 1e25, 1e20, 1e10, 1.0, 1e-10, 1e-30]
 
 
-def far_rows(dtype, rng=None, n=0):
-    """(a, b, dy) of every combination of A_FAR and SIZES, and n drawn ones, as
-    the type holds them, where the 64-bit results fit in it."""
-    a, b, g = (v.reshape(-1) for v in np.meshgrid(A_FAR, SIZES + [-v for v in SIZES], SIZES, indexing="ij"))
-    if n:
-        sign = lambda: rng.choice([-1.0, 1.0], n)  # noqa: E731
-        a = np.concatenate([a, -10.0 ** rng.uniform(-2, 2.8, n)])
-        b = np.concatenate([b, sign() * 10.0 ** rng.uniform(-37, 38, n)])
-        g = np.concatenate([g, sign() * 10.0 ** rng.uniform(-37, 38, n)])
+def far_rows(dtype, rng, n, most):
+    """(a, b, dy) of every combination of A_FAR and SIZES, and n drawn ones, of sizes up
+    to 10^most, as the type holds them."""
+    sizes = [v for v in SIZES if v <= 10.0 ** most]
+    small = [v for v in A_FAR if abs(v) <= 10.0 ** most]
+    a, b, g = (v.reshape(-1) for v in np.meshgrid(small, sizes + [-v for v in sizes], sizes, indexing="ij"))
+    sign = lambda: rng.choice([-1.0, 1.0], n)  # noqa: E731
+    a = np.concatenate([a, -10.0 ** rng.uniform(-2, 2.8, n)])
+    b = np.concatenate([b, sign() * 10.0 ** rng.uniform(-37, most, n)])
+    g = np.concatenate([g, sign() * 10.0 ** rng.uniform(-37, most, n)])
     return [ref.f64(dev(v, dtype)).reshape(-1, 1) for v in (a, b, g)]
 
 
-def check_far(dtype, act, forward, slope):
-    a, b, g = far_rows(dtype, np.random.default_rng(1), 20000)
+def check_far(dtype, act, forward, slope, most=38):
+    a, b, g = far_rows(dtype, np.random.default_rng(1), 4000, most)
     ka, kb = ref.pack(a)[2], ref.pack(b)[2]
     f, bf = forward(a)
     kf, bkf = forward(ka)
     kdf, bdf = slope(ka)
     fits = np.abs(np.stack([f * b, g * kb * kdf, g * kf])).max(0)[:, 0] < 3e38
     a, b, g, kb, f, bf, kf, bkf, kdf, bdf = (v[fits] for v in (a, b, g, kb, f, bf, kf, bkf, kdf, bdf))
-    assert a.shape[0] > 15000
+    assert a.shape[0] > 3000
     y, p = lsmgnn.act8(dev(np.concatenate([a, b], 1), dtype), act, True)
     ref.assert_within(y, f * b, (bf + 2 * ref.U32 * np.abs(f)) * np.abs(b) + LEAST, dtype, "y")
     dx = lsmgnn.act8_grad(dev(g, dtype), p, act, True)
@@ -238,3 +239,30 @@ def test_combine_gradient_of_many_tokens():
     for a in range(0, n, 1 << 23):
         b = min(n, a + (1 << 23))
         assert torch.equal(dz[n - b:n - a].flip(0), dy[a:b])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_factors_that_are_only_small(dtype, act):
+    """Where no factor of a wave is above 2^40 they are multiplied as they are."""
+    if act == "silu":
+        check_far(dtype, "silu", lambda x: ref.act("silu", x)[:2], lambda x: ref.act("silu", x)[2:], 11)
+    else:
+        check_far(dtype, "gelu", lambda x: gelu64(x, dtype), lambda x: gelu_slope64(x, dtype), 11)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_a_large_neighbour_changes_nothing(dtype, act):
+    """A row's results are the same bits whether or not one beside it takes its wave
+    the large numbers' way."""
+    rng = np.random.default_rng(3)
+    x, dy = rows(rng, 64, 96, dtype), rows(rng, 64, 48, dtype)
+    y, p = lsmgnn.act8(x, act, True)
+    dx = lsmgnn.act8_grad(dy, p, act, True)
+    far = x.clone()
+    far[::3, 60] = torch.finfo(dtype).max / 4
+    y_far, p_far = lsmgnn.act8(far, act, True)
+    dx_far = lsmgnn.act8_grad(dy, p_far, act, True)
+    same = torch.arange(64, device="cuda") % 3 != 0
+    assert torch.equal(y_far[same], y[same]) and torch.equal(dx_far[same], dx[same])
