@@ -592,8 +592,9 @@ def _matrix(t, name, dim=None, rows=None, like=None):
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions, not {t.dim()}")
     n, d = t.shape
-    ld = t.stride(0) if n > 1 else max(d, 1)
-    if d > 1 and t.stride(1) != 1 or ld < d:
+    row, column = t.stride()
+    ld = row if n > 1 else max(d, 1)
+    if d > 1 and column != 1 or ld < d:
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
     if dim is not None and d != dim or rows is not None and n != rows:
         raise ValueError(f"{name} must be {rows if rows is not None else n} rows of {dim if dim is not None else d}, "
@@ -603,10 +604,11 @@ def _matrix(t, name, dim=None, rows=None, like=None):
     return t.data_ptr(), n, d, ld, _type_code(t.dtype, name)
 
 
-def _vector(t, dtype, numel, name, device):
-    """Address of a contiguous device tensor of `numel` elements of `dtype`."""
+def _vector(t, dtype, numel, name, device, floats=False):
+    """Address of a contiguous device tensor of `numel` elements of `dtype`, a
+    floating-point one or not."""
     _dev_ptr(t, dtype, name)
-    if t.requires_grad:
+    if floats and t.requires_grad:
         _no_graph(t, name)
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, not {t.numel()}")
@@ -828,7 +830,7 @@ def route_combine(z, plan, weights=None, out=None, stream=None):
     import torch
     device = z.device
     zp, rows, dim, zld, zt = _matrix(z, "z", rows=plan.rows, like=plan.device)
-    wp = None if weights is None else _vector(weights, torch.float32, plan.n * plan.k, "weights", device)
+    wp = None if weights is None else _vector(weights, torch.float32, plan.n * plan.k, "weights", device, True)
     out, op, old, ot = _output(out, "out", plan.n, dim, z.dtype, device, stream)
     if ot != zt:
         raise TypeError("z and out must have one type")
@@ -843,7 +845,7 @@ def route_combine_grad(dy, z, plan, weights, dz=None, stream=None):
     device = dy.device
     dp, n, dim, dld, dt = _matrix(dy, "dy", rows=plan.n, like=plan.device)
     zp, rows, _, zld, zt = _matrix(z, "z", dim, plan.rows, device)
-    wp = _vector(weights, torch.float32, plan.n * plan.k, "weights", device)
+    wp = _vector(weights, torch.float32, plan.n * plan.k, "weights", device, True)
     dz, op, old, ot = _output(dz, "dz", rows, dim, dy.dtype, device, stream)
     if zt != dt or ot != dt:
         raise TypeError("dy, z and dz must have one type")
@@ -966,7 +968,7 @@ def weight_grad8(packed, dy, offsets=None, dtype=None, out=None, work=None, stre
     fp = None if offsets is None else _vector(offsets, torch.int32, experts + 1, "offsets", device)
     if out is None:
         out = _empty((experts, din, dout), dtype or torch.float32, device, stream)
-    op = _vector(out, out.dtype, experts * din * dout, "out", device)
+    op = _vector(out, out.dtype, experts * din * dout, "out", device, True)
     work, wp, wb = _work(weight_grad8_work_bytes(rows, din, dout, experts), work, device, stream)
     _run("lsmgnn_weight_grad8", device, stream, qp, sp, rows, din, dp, dout, dld, dt, fp, experts, op,
          _type_code(out.dtype, "out"), wp, wb)
