@@ -30,10 +30,6 @@ using namespace lsm_rows;
 constexpr int kLane = 8;                            // values per lane
 constexpr int kPack = (int)LSMGNN_PACK_BLOCK;       // values per block
 constexpr int kQuads = kPack / kLane;               // lanes per block
-// places per thread of an activation: their loads are in flight together.  Gated
-// silu of 65537 x 1024 bf16: 98 us with 2, 103 with 1; its gradient, which waits on
-// arithmetic, 100 with 1, 122 with 2.
-constexpr int kActPlaces = 2, kGradPlaces = 1;
 
 // A lane's place: row, block of the row, first element.
 struct Place {
@@ -301,72 +297,60 @@ __device__ __forceinline__ void backward8(const float (&g)[kLane], const float (
   }
 }
 
+// One place a thread, as in the other passes: with two, whose loads are in flight
+// together, gated silu of 65537 x 1024 bf16 takes 96 us instead of 92, its gradient 93
+// instead of 92.
 template <typename T, uint32_t kAct, bool kGated>
 __global__ __launch_bounds__(kBlock) void k_act(Cut c, const T *x, uint64_t xld, T *y, uint64_t yld, int8_t *q,
                                                 uint8_t *scale) {
   constexpr int kRows = kGated ? 2 : 1;  // kept rows of a row
-  Place p[kActPlaces];
-  float a[kActPlaces][kLane], b[kActPlaces][kLane];
-#pragma unroll
-  for (int u = 0; u < kActPlaces; ++u) {
-    p[u] = place_of(c, (uint64_t)blockIdx.x * (kBlock * kActPlaces), u * kBlock + threadIdx.x);
-    const T *row = x + p[u].row * xld + p[u].col;
-    load8(row, p[u].count, a[u]);
-    if (kGated) load8(row + c.dim, p[u].count, b[u]);
+  const Place p = place_of(c, (uint64_t)blockIdx.x * kBlock, threadIdx.x);
+  float a[kLane], b[kLane], o[kLane];
+  const T *row = x + p.row * xld + p.col;
+  load8(row, p.count, a);
+  if (kGated) load8(row + c.dim, p.count, b);
+  const uint32_t big_a = largest(a), big_b = kGated ? largest(b) : 0;
+  if (__any((big_a > big_b ? big_a : big_b) >= __float_as_uint(kNear))) {
+    rarely();
+    forward8<kAct, T, kGated, true>(a, b, o);
+  } else {
+    forward8<kAct, T, kGated, false>(a, b, o);
   }
-#pragma unroll
-  for (int u = 0; u < kActPlaces; ++u) {
-    float o[kLane];
-    const uint32_t big_a = largest(a[u]), big_b = kGated ? largest(b[u]) : 0;
-    if (__any((big_a > big_b ? big_a : big_b) >= __float_as_uint(kNear))) {
-      rarely();
-      forward8<kAct, T, kGated, true>(a[u], b[u], o);
-    } else {
-      forward8<kAct, T, kGated, false>(a[u], b[u], o);
-    }
-    if (p[u].count) store8(y + p[u].row * yld + p[u].col, p[u].count, o);
-    int8_t *qp = q + p[u].row * kRows * c.dim + p[u].col;
-    uint8_t *sp = scale + p[u].row * kRows * c.nb + p[u].block;
-    keep8(a[u], p[u], qp, sp);
-    if (kGated) keep8(b[u], p[u], qp + c.dim, sp + c.nb);
-  }
+  if (p.count) store8(y + p.row * yld + p.col, p.count, o);
+  int8_t *qp = q + p.row * kRows * c.dim + p.col;
+  uint8_t *sp = scale + p.row * kRows * c.nb + p.block;
+  keep8(a, p, qp, sp);
+  if (kGated) keep8(b, p, qp + c.dim, sp + c.nb);
 }
 
 template <typename T, uint32_t kAct, bool kGated>
 __global__ __launch_bounds__(kBlock) void k_act_grad(Cut c, const T *dy, uint64_t dyld, const int8_t *q,
                                                      const uint8_t *scale, T *dx, uint64_t dxld) {
   constexpr int kRows = kGated ? 2 : 1;
-  Place p[kGradPlaces];
-  float g[kGradPlaces][kLane], a[kGradPlaces][kLane], b[kGradPlaces][kLane];
+  const Place p = place_of(c, (uint64_t)blockIdx.x * kBlock, threadIdx.x);
+  float g[kLane], a[kLane], b[kLane], o[kLane];
+  const int8_t *qp = q + p.row * kRows * c.dim + p.col;
+  const uint8_t *sp = scale + p.row * kRows * c.nb + p.block;
+  load8(dy + p.row * dyld + p.col, p.count, g);
+  kept8(qp, sp, p.count, a);
+  if (kGated) kept8(qp + c.dim, sp + c.nb, p.count, b);
+  float big = 0.0f;  // a NaN is no larger: it comes through either way
+  if (kWide<T>)
 #pragma unroll
-  for (int u = 0; u < kGradPlaces; ++u) {
-    p[u] = place_of(c, (uint64_t)blockIdx.x * (kBlock * kGradPlaces), u * kBlock + threadIdx.x);
-    const int8_t *qp = q + p[u].row * kRows * c.dim + p[u].col;
-    const uint8_t *sp = scale + p[u].row * kRows * c.nb + p[u].block;
-    load8(dy + p[u].row * dyld + p[u].col, p[u].count, g[u]);
-    kept8(qp, sp, p[u].count, a[u]);
-    if (kGated) kept8(qp + c.dim, sp + c.nb, p[u].count, b[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < kGradPlaces; ++u) {
-    float o[kLane], big = 0.0f;  // a NaN is no larger: it comes through either way
-    if (kWide<T>)
-#pragma unroll
-      for (int e = 0; e < kLane; ++e) {
-        big = fmaxf(fmaxf(big, fabsf(g[u][e])), fabsf(a[u][e]));
-        if (kGated) big = fmaxf(big, fabsf(b[u][e]));
-      }
-    if (__any(big >= kNear)) {
-      rarely();
-      backward8<kAct, T, kGated, true>(g[u], a[u], b[u], o);
-    } else {
-      backward8<kAct, T, kGated, false>(g[u], a[u], b[u], o);
+    for (int e = 0; e < kLane; ++e) {
+      big = fmaxf(fmaxf(big, fabsf(g[e])), fabsf(a[e]));
+      if (kGated) big = fmaxf(big, fabsf(b[e]));
     }
-    if (p[u].count == 0) continue;
-    T *to = dx + p[u].row * dxld + p[u].col;
-    store8(to, p[u].count, o);
-    if (kGated) store8(to + c.dim, p[u].count, b[u]);
+  if (__any(big >= kNear)) {
+    rarely();
+    backward8<kAct, T, kGated, true>(g, a, b, o);
+  } else {
+    backward8<kAct, T, kGated, false>(g, a, b, o);
   }
+  if (p.count == 0) return;
+  T *to = dx + p.row * dxld + p.col;
+  store8(to, p.count, o);
+  if (kGated) store8(to + c.dim, p.count, b);
 }
 
 Cut cut_of(uint64_t rows, uint64_t dim) {
@@ -379,7 +363,7 @@ Cut cut_of(uint64_t rows, uint64_t dim) {
   return c;
 }
 
-uint64_t blocks_of(const Cut &c, int per = 1) { return blocks_for(c.rows * c.nb * kQuads, kBlock * per); }
+uint64_t blocks_of(const Cut &c) { return blocks_for(c.rows * c.nb * kQuads, kBlock); }
 
 // f(cut, first row) for launches of all rows.
 template <typename F>
@@ -1015,8 +999,8 @@ lsmgnn_status lsmgnn_act8(const void *x, uint64_t rows, uint64_t dim, uint64_t x
     typedef typename decltype(tag)::T T;
     with_act(act, gated, [&](auto f, auto g) {
       cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
-        hipLaunchKernelGGL((k_act<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kActPlaces)),
-                           dim3(kBlock), 0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(x) + r * x_ld,
+        hipLaunchKernelGGL((k_act<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c)), dim3(kBlock),
+                           0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(x) + r * x_ld,
                            x_ld, static_cast<T *>(y) + r * y_ld, y_ld, q + r * kept * dim, scale + r * kept * c.nb);
       });
     });
@@ -1039,8 +1023,8 @@ lsmgnn_status lsmgnn_act8_grad(const void *dy, uint64_t rows, uint64_t dim, uint
     typedef typename decltype(tag)::T T;
     with_act(act, gated, [&](auto f, auto g) {
       cuts_of(rows, dim, [&](const Cut &c, uint64_t r) {
-        hipLaunchKernelGGL((k_act_grad<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c, kGradPlaces)),
-                           dim3(kBlock), 0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(dy) + r * dy_ld,
+        hipLaunchKernelGGL((k_act_grad<T, decltype(f)::value, decltype(g)::value>), dim3(blocks_of(c)), dim3(kBlock),
+                           0, static_cast<hipStream_t>(stream), c, static_cast<const T *>(dy) + r * dy_ld,
                            dy_ld, q + r * kept * dim, scale + r * kept * c.nb, static_cast<T *>(dx) + r * dx_ld, dx_ld);
       });
     });
