@@ -161,9 +161,9 @@ __device__ __forceinline__ void sort_items(Place (&item)[kN], const bool (&ok)[k
   }
 }
 
-// At most 1024 * kN places, sorted by block 0; the others fill (see Fill).  With
-// more places (14000, 64 bf16 of 100000 rows) it takes 80 us where the tiles of
-// sort.h take 73; with 3000 it is 60 against 67.
+// At most 1024 * kN places, sorted by block 0; the others fill (see Fill).  The gradient
+// by rows of 64 bf16 out of 100000 so, and by the tiles of sort.h: 1000 places 20 and
+// 24 us, 3000 26 and 35, 4096 28 and 35.
 template <int kN>
 __global__ __launch_bounds__(kSortThreads) void k_sort_block(FromIds src, uint32_t n, uint32_t key_bits, Place *out,
                                                              lsm_sort::Fill fill) {
@@ -210,7 +210,10 @@ __global__ __launch_bounds__(kBlock) void k_count_heads(const Place *places, uin
 }
 
 // With many tiles, how many begin before each: one block, so that the blocks of the
-// sums, which otherwise add up the tiles before them, need not read them all.
+// sums, which otherwise add up the tiles before them, need not read them all, a
+// square of the places in all.  Rows of 8 bf16, scanned and not: 4 million places 543
+// and 537 us, 5 million 684 and 677, 10 million 1309 and 1315, 20 million 2688 and
+// 2707.
 constexpr uint32_t kScannedHeads = 4096;
 
 __global__ __launch_bounds__(kSortThreads) void k_scan_heads(uint32_t *heads, uint32_t tiles) {
@@ -532,7 +535,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_runs(Sums s, uint32_t chu
 // as k_sum_runs does, and a run that crosses shares is joined through LDS.  The
 // rows that no ID names are written by blocks of consecutive rows, from a bit a
 // row that the same look at the IDs sets.  Bound by this chain, not by bytes: 9001
-// places of 128 f32 in 13.8 us, where reading the IDs ends at 6 and the rows take 4;
+// places of 128 f32 in 13.5 us, where reading the IDs ends at 6 and the rows take 4;
 // 12288 take 15.5 us, and 12289 by the sort, the sums and the join 33.
 constexpr uint64_t kFewPlaces = 1024 * 12;
 constexpr uint32_t kFewBlocks = 256, kFewZeroRows = 1u << 16;
@@ -868,7 +871,8 @@ void queue_few_places(Sums s, const void *dy, uint32_t dy_type, const int64_t *i
     // Parts of 16 loads cost narrow rows more than they save (16384 x 128 f32, 9001
     // IDs: 13.6 us uncut, 15.0 so)
     uint32_t split = 0;
-    while ((2u << split) <= kFewBlocks && all >> (split + 1) >= kFewUnits && ((uint64_t)s.n << (split + 1)) <= (uint64_t)kFewShare * kFewBlocks)
+    while ((2u << split) <= kFewBlocks && all >> (split + 1) >= kFewUnits &&
+           ((uint64_t)s.n << (split + 1)) <= (uint64_t)kFewShare * kFewBlocks)
       ++split;
     const uint32_t units = (all + (1u << split) - 1) >> split;
     s.lanes_shift = lanes_shift(units);

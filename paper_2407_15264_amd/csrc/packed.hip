@@ -13,8 +13,9 @@
 // The passes over rows are bound by memory.  A lane takes 8 consecutive values, a
 // block of 32 is four neighbouring lanes', and the largest magnitude crosses them
 // in two exchanges.  Measured: 203003 x 1024 bf16 kept in 112 us, 5.6 TB/s read and
-// written; gated silu of 65537 x 1024 bf16 in 95 us with its kept input, its
-// gradient in 92 us (5.7 and 5.9).
+// written, and read back in 88; gated silu of 65537 x 1024 bf16 in 93 us with its kept
+// input, its gradient in 90 (5.8 and 6.0), gelu in 98 and 103, which its arithmetic
+// bounds.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -389,8 +390,10 @@ void cuts_of(uint64_t rows, uint64_t dim, F f) {
 //
 // Measured: 1024 x 256 of 203003 rows bf16 in 136 to 152 us, 700 to 780 TFLOP/s, the
 // second kernel 13 us; a product of large bf16 matrices reaches 1140.  Staging (the
-// widening and the turning over), LDS and the matrix units take about equal times and
-// overlap in part.
+// widening and the turning over) bounds it, unevenly: in steps of 32 rows a tile of 256
+// has units of x for half of the threads, whose waves the others wait for, and so have
+// a tile of 128 with dy in several parts and one of 64.  The threads without a unit
+// load past the buffer's end, that is nothing.
 
 constexpr uint32_t kXcds = 8;
 
@@ -523,7 +526,9 @@ template <typename T, int kM, int kN, int kWavesM, int kWavesN>
 struct Tile {
   static constexpr int kThreads = 64 * kWavesM * kWavesN;
   static constexpr int kP = kParts<T>;
-  // rows per step: two steps' pieces of both operands fit in LDS
+  // rows per step: two steps' pieces of both operands in 64 KiB of LDS.  There is more
+  // of it, but 64 rows of the 256 tile take more registers than there are: 1024 x 256
+  // of 203003 rows bf16 150 us, 298 so
   static constexpr int kK = (kM + kP * kN) * 64 * 2 * 2 <= 65536 ? 64 : 32;
   static constexpr int kPieces = kK / 8;       // pieces of a column in a step
   static constexpr int kCols = 16 / kPieces;   // columns per line of LDS

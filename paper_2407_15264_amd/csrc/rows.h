@@ -143,8 +143,8 @@ __device__ __forceinline__ void store_row(T *p, const T (&v)[kN]) {
 // where they do not share lines.  Row
 // sums 780 / 788 / 788 / 754 (900000 x 1024 f16), 119 / 123 / 117 / 123 (123457 x
 // 256 bf16), 142 / 144 / 144 / 152 (300000 x 257): both where the rows are more
-// than the last-level cache, else none.  Activations 204 / 205 /
-// 192 / 191 (200000 x 257 gated bf16, forward and backward): both.
+// than the last-level cache, else none.  Activations 203 / 208 /
+// 192 / 190 (200000 x 257 gated bf16, forward and backward): both.
 template <int kN, typename T>
 __device__ __forceinline__ void load_row_once(const T *p, T (&v)[kN]) {
   typedef typename PieceOf<sizeof(v)>::V V;
