@@ -266,3 +266,18 @@ def test_a_large_neighbour_changes_nothing(dtype, act):
     dx_far = lsmgnn.act8_grad(dy, p_far, act, True)
     same = torch.arange(64, device="cuda") % 3 != 0
     assert torch.equal(y_far[same], y[same]) and torch.equal(dx_far[same], dx[same])
+
+
+@pytest.mark.parametrize("n", [0, 5, 13_000])
+def test_gradient_of_more_than_one_launch_clears(n):
+    """A whole gradient of 65 GiB: no row keeps what was there."""
+    room_for(80)
+    num_rows, dim = 33_300_000, 1024
+    grad = torch.ones((num_rows, dim), dtype=torch.bfloat16, device="cuda")
+    ids = torch.arange(n, device="cuda") * 2500 + 7
+    dy = torch.full((n, dim), 2.0, dtype=torch.bfloat16, device="cuda")
+    lsmgnn.embed_grad(dy, ids, num_rows, grad=grad)
+    assert bool((grad[ids] == 2).all())
+    grad[ids] = 0
+    for a in range(0, num_rows, 4_000_000):
+        assert not grad[a:a + 4_000_000].any()
